@@ -43,11 +43,16 @@ __device__ __forceinline__ int key_count(const CrossArgs& a, int b) {
 // The work item of a workgroup.  Workgroup ids go round-robin over the 8 XCDs: each XCD takes one eighth of the items in their
 // order (all items of a key head one after the other), so that the workgroups that run together on it read the same keys.
 __device__ __forceinline__ bool cross_item(const CrossArgs& a, uint32_t& item) {
-  const uint32_t per = gridDim.x / N_XCD;
-  item = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  const uint32_t per = gridDim.x * gridDim.y / N_XCD, id = blockIdx.y * gridDim.x + blockIdx.x;
+  item = (id & 7) * per + (id >> 3);
   return item < (uint32_t)a.total;
 }
-inline unsigned cross_grid(long long total) { return (unsigned)((total + N_XCD - 1) / N_XCD * N_XCD); }
+// A launch dimension stays below 2^32 threads: 2^23 workgroups of 256 in x, the others in y (2^30 fp32 rows are 2^24 workgroups).
+constexpr long long GRID_X = 1ll << 23;
+inline dim3 cross_grid(long long total) {
+  const long long y = (total + GRID_X - 1) / GRID_X, x = ((total + y - 1) / y + N_XCD - 1) / N_XCD * N_XCD;
+  return dim3((unsigned)x, (unsigned)y);
+}
 
 // How a call is cut.  Chosen from the problem alone, so that the workspace can be sized by it.
 struct CrossPlan {

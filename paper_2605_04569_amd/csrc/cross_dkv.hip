@@ -246,7 +246,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_dkv(CrossArgs a
 }
 
 hipError_t launch_cross_dkv(const CrossArgs& a, int D, hipStream_t st) {
-  const dim3 grid(cross_grid(a.total)), blk(256);
+  const dim3 grid = cross_grid(a.total), blk(256);
   if (D == 128) hipLaunchKernelGGL(k_cross_dkv<128>, grid, blk, 0, st, a);
   else hipLaunchKernelGGL(k_cross_dkv<64>, grid, blk, 0, st, a);
   return hipGetLastError();

@@ -261,7 +261,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_dq(CrossArgs a)
 }
 
 hipError_t launch_cross_dq(const CrossArgs& a, int D, hipStream_t st) {
-  const dim3 grid(cross_grid(a.total)), blk(256);
+  const dim3 grid = cross_grid(a.total), blk(256);
   if (D == 128) hipLaunchKernelGGL(k_cross_dq<128>, grid, blk, 0, st, a);
   else hipLaunchKernelGGL(k_cross_dq<64>, grid, blk, 0, st, a);
   return hipGetLastError();

@@ -263,19 +263,19 @@ __global__ __launch_bounds__(256, 2) void k_cross_dkv_f32(CrossArgs a) {
 }
 
 hipError_t launch_cross_forward_f32(const CrossArgs& a, int D, hipStream_t st) {
-  const dim3 grid(cross_grid(a.total)), blk(256);
+  const dim3 grid = cross_grid(a.total), blk(256);
   if (D == 128) hipLaunchKernelGGL((k_cross_rows_f32<128, false>), grid, blk, 0, st, a);
   else hipLaunchKernelGGL((k_cross_rows_f32<64, false>), grid, blk, 0, st, a);
   return hipGetLastError();
 }
 hipError_t launch_cross_dq_f32(const CrossArgs& a, int D, hipStream_t st) {
-  const dim3 grid(cross_grid(a.total)), blk(256);
+  const dim3 grid = cross_grid(a.total), blk(256);
   if (D == 128) hipLaunchKernelGGL((k_cross_rows_f32<128, true>), grid, blk, 0, st, a);
   else hipLaunchKernelGGL((k_cross_rows_f32<64, true>), grid, blk, 0, st, a);
   return hipGetLastError();
 }
 hipError_t launch_cross_dkv_f32(const CrossArgs& a, int D, hipStream_t st) {
-  const dim3 grid(cross_grid(a.total)), blk(256);
+  const dim3 grid = cross_grid(a.total), blk(256);
   if (D == 128) hipLaunchKernelGGL(k_cross_dkv_f32<128>, grid, blk, 0, st, a);
   else hipLaunchKernelGGL(k_cross_dkv_f32<64>, grid, blk, 0, st, a);
   return hipGetLastError();

@@ -536,7 +536,7 @@ hipError_t launch_cross_forward(CrossArgs a, const isa_cross_problem& p, hipStre
     e = launch_cross_forward_f32(a, p.D, st);
   } else {
     const bool lse = a.lse != nullptr;
-    const dim3 grid(c.narrow ? (unsigned)a.total : cross_grid(a.total)), blk(256);
+    const dim3 grid = c.narrow ? dim3((unsigned)a.total) : cross_grid(a.total), blk(256);
 #define ISA_CROSS(kernel, D)                                                                 \
   do {                                                                                       \
     if (lse) hipLaunchKernelGGL((kernel<D, true>), grid, blk, 0, st, a);                     \

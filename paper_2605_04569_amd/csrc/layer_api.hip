@@ -73,7 +73,7 @@ static int check_cross(const isa_cross_problem* p) {
   if (p->D != 64 && p->D != 128) return ISA_ERR_SHAPE;
   if (p->B < 0 || p->H < 1 || p->H_kv < 1 || p->H % p->H_kv) return ISA_ERR_SHAPE;
   if (p->S_q < 0 || p->S_k < 0 || p->S_q > (1 << 28) || p->S_k > (1 << 28)) return ISA_ERR_SHAPE;
-  const long long bh = (long long)p->B * p->H;             // (launches stay below 2^32 threads)
+  const long long bh = (long long)p->B * p->H;             // (no count of rows or workgroups passes 31 bits)
   if (bh > (1 << 20) || bh * p->S_q > (1 << 30) || bh / (p->H / p->H_kv) * p->S_k > (1 << 30)) return ISA_ERR_SHAPE;
   if (!(p->scale > 0.0) || !isfinite(p->scale) || !isfinite((float)(p->scale * 1.4426950408889634)) || !((float)p->scale > 0.0f))
     return ISA_ERR_UNSUPPORTED;
