@@ -299,8 +299,8 @@ typedef struct isa_cross_problem {
 } isa_cross_problem;
 
 /* Host only.  Bytes of 256-byte aligned workspace that isa_cross_attention (backward = 0: at most 70 MB) or isa_cross_attention_backward
- * (1: at most 300 MB, and 8 bytes for every row of q) needs; scratch, undefined before and after; 0 if `p` is invalid (and where none is
- * needed: such a call takes NULL). */
+ * (1: at most 300 MB, and 512 bytes for every 64 queries, the last fewer ones of a head included) needs; scratch, undefined before and
+ * after; 0 if `p` is invalid (and where none is needed: such a call takes NULL). */
 size_t isa_cross_workspace_bytes(const isa_cross_problem* p, int backward);
 
 /* out[b, h, i] = sum_j P_ij v[b, h', j], P = softmax over the valid j of scale q[b, h, i] . k[b, h', j].

@@ -1,4 +1,4 @@
-// How cross attention's host side cuts its work, checked without a GPU: grids over the whole range of item counts.
+// How cross attention's host side cuts its work, checked without a GPU: grids over the whole range of item counts, workspaces.
 // (tests/test_cross_host.py builds and runs this.)
 #include <stdio.h>
 
@@ -20,6 +20,24 @@ int main() {
     const long long all = (long long)g.x * g.y;
     EXPECT(all >= total && all < total + 8 * 4);
   }
+  // The workspace stays within what the header names, over a spread of problems up to its limits, single queries of many heads among them
+  for (int dtype = 0; dtype < 2; ++dtype)
+    for (int D = 64; D <= 128; D += 64)
+      for (int B : {1, 3, 8, 1000, 1 << 20})
+        for (int H_kv : {1, 2, 5, 40, 65535, 1 << 20})
+          for (int g : {1, 2, 5})
+            for (int S_q : {1, 2, 16, 17, 63, 64, 65, 129, 1000, 65520, 1 << 20, 1 << 28})
+              for (int S_k : {0, 1, 77, 128, 129, 1000, 16384, 1 << 20, 1 << 28}) {
+                const long long bh = (long long)B * H_kv * g;
+                if (bh > (1 << 20) || bh * S_q > (1 << 30) || (long long)B * H_kv * S_k > (1 << 30)) continue;
+                isa_cross_problem p = {};
+                p.B = B; p.H = H_kv * g; p.H_kv = H_kv; p.D = D; p.S_q = S_q; p.S_k = S_k; p.dtype = dtype; p.scale = 0.125;
+                const isa_strides q = {(int64_t)p.H * S_q * D, (int64_t)S_q * D, D}, k = {(int64_t)H_kv * (S_k + 1) * D, (int64_t)(S_k + 1) * D, D};
+                p.q = p.out = p.d_out = p.dq = q;
+                p.k = p.v = p.dk = p.dv = k;
+                const size_t f = isa_cross_workspace_bytes(&p, 0), b = isa_cross_workspace_bytes(&p, 1);
+                EXPECT(f <= 70000000u && b > 0 && b <= 300000000u + 512ull * bh * ((S_q + 63) / 64));
+              }
   printf("%s (%d failures)\n", failures ? "FAILED" : "host checks ok", failures);
   return failures ? 1 : 0;
 }
