@@ -62,6 +62,7 @@ struct CrossPlan {
   size_t part_rows;                 // rows of partial results
 };
 CrossPlan cross_forward_plan(const isa_cross_problem& p);
+bool cross_states_streamed(const isa_cross_problem& p);      // narrow: keys and values are loaded past the caches
 struct CrossBackwardPlan {
   int dq_rows, dq_items, dq_parts;  // query rows of a workgroup
   int kv_rows, kv_items, kv_parts;  // keys of a workgroup

@@ -300,6 +300,7 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossArgs a) {
 // STREAM: keys and values are loaded past the caches, which is quicker where those cannot keep them from call to call (more than 256 MB, the size of the
 // cache in front of the memory): 8 rows over 16 384 states of 8 heads, 537 MB 103 -> 89 us (6.0 TB/s), 1074 MB 185 -> 161 (6.7).  268 MB: 46 -> 48 us if
 // they were read the call before, 56 -> 49 if not.
+// States that several batch items or heads share (a stride of 0) count once.
 constexpr long long KEPT_BYTES = 256ll << 20;
 template <int D, bool LSE, bool STREAM>
 __global__ __launch_bounds__(256, 2) void k_cross_narrow(CrossArgs a) {
@@ -514,6 +515,13 @@ CrossPlan cross_forward_plan(const isa_cross_problem& p) {
   return c;
 }
 
+bool cross_states_streamed(const isa_cross_problem& p) {
+  long long bytes = 0;
+  for (const isa_strides* s : {&p.k, &p.v})
+    bytes += 2ll * p.D * (s->b ? p.B : 1) * (s->h ? p.H_kv : 1) * (s->t ? p.S_k : 1);
+  return bytes > KEPT_BYTES;
+}
+
 template <typename T> static hipError_t merge(const CrossArgs& a, int D, int tile_rows, hipStream_t st) {
   const long long rows = (long long)a.B * a.Hkv * a.rows;
   const int groups = 256 / (D / 4);
@@ -548,7 +556,7 @@ hipError_t launch_cross_forward(CrossArgs a, const isa_cross_problem& p, hipStre
     else hipLaunchKernelGGL((k_cross_narrow<D, LSE, false>), grid, blk, 0, st, a);                        \
   } while (0)
     if (c.narrow) {
-      const bool stream = (long long)p.B * p.H_kv * p.S_k * p.D * 4 > KEPT_BYTES;
+      const bool stream = cross_states_streamed(p);
       if (p.D == 128) { if (lse) ISA_NARROW(128, true); else ISA_NARROW(128, false); }
       else { if (lse) ISA_NARROW(64, true); else ISA_NARROW(64, false); }
     } else {

@@ -1,4 +1,4 @@
-// How cross attention's host side cuts its work, checked without a GPU: grids over the whole range of item counts, workspaces.
+// How cross attention's host side cuts its work, checked without a GPU: grids over the whole range of item counts, workspaces, which states are streamed.
 // (tests/test_cross_host.py builds and runs this.)
 #include <stdio.h>
 
@@ -38,6 +38,27 @@ int main() {
                 const size_t f = isa_cross_workspace_bytes(&p, 0), b = isa_cross_workspace_bytes(&p, 1);
                 EXPECT(f <= 70000000u && b > 0 && b <= 300000000u + 512ull * bh * ((S_q + 63) / 64));
               }
+  // Single queries stream their states where the distinct ones are more than 256 MB: eight requests on one document of 67 MB do not
+  {
+    isa_cross_problem p = {};
+    p.B = 8; p.H = 40; p.H_kv = 8; p.D = 128; p.S_q = 1; p.S_k = 16384; p.scale = 0.1;
+    p.k = p.v = isa_strides{8ll * 16384 * 128, 16384 * 128, 128};
+    EXPECT(cross_states_streamed(p));
+    p.k.b = 0;
+    EXPECT(cross_states_streamed(p));                      // (the values alone: 268 MB, and 34 MB of keys)
+    p.v.b = 0;
+    EXPECT(!cross_states_streamed(p));
+    p.B = 64;
+    EXPECT(!cross_states_streamed(p));
+    p.S_k = 1 << 17;
+    EXPECT(cross_states_streamed(p));                      // one document of 537 MB
+    p.k.h = p.v.h = 0;
+    EXPECT(!cross_states_streamed(p));
+    p.B = 1; p.H_kv = 1; p.S_k = 1 << 19;
+    EXPECT(!cross_states_streamed(p));                     // 256 MB
+    p.S_k += 1;
+    EXPECT(cross_states_streamed(p));
+  }
   printf("%s (%d failures)\n", failures ? "FAILED" : "host checks ok", failures);
   return failures ? 1 : 0;
 }
