@@ -31,9 +31,13 @@ def _like(t):
     return torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
+_LENGTHS = (torch.int32, torch.int64, torch.int16, torch.int8, torch.uint8)      # what becomes 32 bits without changing its meaning
+
+
 def _masks(q, k, kv_len, key_mask):
     if kv_len is not None:
-        B._require(kv_len.shape == (q.shape[0],) and kv_len.is_cuda and not kv_len.is_floating_point(), "kv_len: one whole number a batch item, on the GPU")
+        B._require(kv_len.dtype in _LENGTHS, "kv_len: whole numbers, signed or bytes")
+        B._require(kv_len.shape == (q.shape[0],) and kv_len.is_cuda, "kv_len: one whole number a batch item, on the GPU")
         if kv_len.dtype == torch.int64:
             kv_len = kv_len.clamp(0, k.shape[2])
         kv_len = kv_len.to(torch.int32).contiguous()
