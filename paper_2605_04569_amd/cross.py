@@ -31,15 +31,15 @@ def _like(t):
     return torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
-_LENGTHS = (torch.int32, torch.int64, torch.int16, torch.int8, torch.uint8)      # what becomes 32 bits without changing its meaning
+_LENGTHS = (torch.int32, torch.int64, torch.int16, torch.int8, torch.uint8, torch.uint16, torch.uint32)      # what 64 bits hold
 
 
 def _masks(q, k, kv_len, key_mask):
     if kv_len is not None:
-        B._require(kv_len.dtype in _LENGTHS, "kv_len: whole numbers, signed or bytes")
+        B._require(kv_len.dtype in _LENGTHS, "kv_len: whole numbers, unsigned ones up to 32 bits")
         B._require(kv_len.shape == (q.shape[0],) and kv_len.is_cuda, "kv_len: one whole number a batch item, on the GPU")
-        if kv_len.dtype == torch.int64:
-            kv_len = kv_len.clamp(0, k.shape[2])
+        if kv_len.dtype in (torch.int64, torch.uint32):
+            kv_len = kv_len.to(torch.int64).clamp(0, k.shape[2])
         kv_len = kv_len.to(torch.int32).contiguous()
     if key_mask is not None:
         B._require(key_mask.shape == (q.shape[0], k.shape[2]) and key_mask.is_cuda and key_mask.dtype in (torch.bool, torch.uint8),
