@@ -228,7 +228,10 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_dkv(CrossArgs a
   for (int kt = 0; kt < 2; ++kt) {
     f32x4 rk[CT], rv[CT];
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) { rk[ct] = ak[ct][kt]; rv[ct] = av[ct][kt]; }
+    for (int ct = 0; ct < CT; ++ct) {                                      // (0 times an infinite gradient is no zero)
+      rk[ct] = kbias[kt][0] == 0.f ? ak[ct][kt] : f32x4{0.f, 0.f, 0.f, 0.f};
+      rv[ct] = kbias[kt][0] == 0.f ? av[ct][kt] : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
     if (a.parts > 1) {
       const long long row = ((long long)bh * a.items + key0 / 128) * a.parts + part;
       float* to = a.part_o + (row * 256 + wave * 32 + 16 * kt + r16) * D;

@@ -124,13 +124,14 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_dq(CrossArgs a)
       for (int qt = 0; qt < 2; ++qt) { settled(as[ct][qt]); settled(ap[ct][qt]); }
 #pragma unroll
     for (int qt = 0; qt < 2; ++qt) {
-      const float es = sum_over_q(e[qt]);
+      const bool none = nlse[qt] == -INFINITY;                             // no valid key: zeros (0 times an infinite gradient is no zero)
+      const float es = none ? 0.f : sum_over_q(e[qt]), ndq = none ? 0.f : nd[qt];
       const RowOf row(a, hk, of_tile * 128, wave * 32 + 16 * qt + r16);
       const bool whole = a.parts == 1;
       if (part == 0 && q == 0 && row.ok) {
         float* s = a.side + (((long long)b * a.H + row.head) * a.side_tiles + (row.query >> 6)) * 128 + (row.query & 63);
         s[0] = nlse[qt];
-        s[64] = whole ? nd[qt] - es : nd[qt];
+        s[64] = whole ? ndq - es : ndq;
         if (row.query == a.Sq - 1)                                         // the places behind the last query: weight 0
           for (int i = 1; i < 64 - (row.query & 63); ++i) { s[i] = -INFINITY; s[64 + i] = 0.f; }
       }
@@ -138,15 +139,15 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_dq(CrossArgs a)
         const long long at = ((long long)slot * a.parts + part) * 128 + wave * 32 + 16 * qt + r16;
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-          *reinterpret_cast<f32x4*>(a.part_o + 2 * at * D + 16 * ct + 4 * q) = as[ct][qt];
-          *reinterpret_cast<f32x4*>(a.part_o + (2 * at + 1) * D + 16 * ct + 4 * q) = ap[ct][qt];
+          *reinterpret_cast<f32x4*>(a.part_o + 2 * at * D + 16 * ct + 4 * q) = none ? zero4 : as[ct][qt];
+          *reinterpret_cast<f32x4*>(a.part_o + (2 * at + 1) * D + 16 * ct + 4 * q) = none ? zero4 : ap[ct][qt];
         }
         if (q == 0) a.part_ml[at] = make_float4(es, 0.f, 0.f, 0.f);
         continue;
       }
       f32x4 r[CT];
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) r[ct] = as[ct][qt] - ap[ct][qt] * es;
+      for (int ct = 0; ct < CT; ++ct) r[ct] = none ? zero4 : as[ct][qt] - ap[ct][qt] * es;
       store_row<D>(r, a.scale, reinterpret_cast<uint16_t*>(a.dq) + at_row(a.sdq, b, row.head, row.query), q, row.ok);
     }
   };

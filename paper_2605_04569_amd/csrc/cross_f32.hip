@@ -175,6 +175,10 @@ __global__ __launch_bounds__(256, 2) void k_cross_rows_f32(CrossArgs a) {
     }
   }
   if (!BWD) l = sum_over_q(l);
+  if (BWD && neg_m == -INFINITY) {                       // no valid key: zeros (0 times an infinite gradient is no zero)
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) acc[ct] = zero4;
+  }
   if (a.parts > 1) {
     const long long at = (slot * a.parts + part) * 64 + wave * 16 + r16;
     store_own<D>(acc, 1.0f, a.part_o + at * D, q);
@@ -218,7 +222,9 @@ __global__ __launch_bounds__(256, 2) void k_cross_dkv_f32(CrossArgs a) {
   const f32x4 zero4 = {0.f, 0.f, 0.f, 0.f};
 
   // tiles of 32 queries: two of each of the 64 that share a place in `side`
-  const int per_head = 2 * a.side_tiles, units = key0 < n_keys ? a.group * per_head : 0;
+  bool any = key0 < n_keys;                               // a block without a valid key streams nothing
+  if (any && mask_row) any = __syncthreads_or(live) != 0;
+  const int per_head = 2 * a.side_tiles, units = any ? a.group * per_head : 0;
   const int u_begin = (int)((long long)units * part / a.parts), u_end = (int)((long long)units * (part + 1) / a.parts);
   TileRegs<D> rq, ro;
   float rs = 0.f;
@@ -250,6 +256,10 @@ __global__ __launch_bounds__(256, 2) void k_cross_dkv_f32(CrossArgs a) {
       add_rows<D>(ot_, p, rt, r16, q, av);
       add_rows<D>(qt_, w, rt, r16, q, ak);
     }
+  }
+  if (!live) {
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) ak[ct] = av[ct] = zero4;
   }
   if (a.parts > 1) {
     const long long at = (((long long)bh * a.items + key0 / 64) * a.parts + part) * 128 + wave * 16 + r16;
