@@ -87,7 +87,6 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_dq(CrossArgs a)
       }
     }
   };
-  constexpr int ROW_LOADS = 2 * KS * 3;                                    // of load_rows, without the two of the log-sum-exps
   auto take_rows = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int qt = 0; qt < 2; ++qt) {
@@ -175,8 +174,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_dq(CrossArgs a)
   for (;;) {
   if (!AHEAD) load_rows(tile);
   take_rows();
-  bool ahead = AHEAD && tile + 1 < tile_end;                               // the next row tile's rows are on their way
-  if (ahead) load_rows(tile + 1);
+  if (AHEAD && tile + 1 < tile_end) load_rows(tile + 1);                   // the next row tile's rows are on their way
   f32x4 as[CT][2], ap[CT][2];
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct)
@@ -226,11 +224,10 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_dq(CrossArgs a)
 #pragma unroll
     for (int hh = 0; hh < 2; ++hh) {
       if (hh == 1) {
-        // All but the newest loads (tile i + 2's and, in a row tile's first iteration, the rows' before them) have landed: tile i + 1 is complete, for
-        // everybody behind the barrier, and everybody is through tile i - 1.
-        if (ahead) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(LOADS + ROW_LOADS) : "memory");
-        else asm volatile("s_waitcnt vmcnt(%0)" :: "n"(LOADS) : "memory");
-        ahead = false;
+        // All but the newest loads (tile i + 2's) have landed: tile i + 1 is complete, for everybody behind the barrier, and everybody is through
+        // tile i - 1.  In a row tile's first iteration this waits for the next row tile's rows too, which went before tile i + 2: their number
+        // is the compiler's to choose, and a wait that allowed for it would be sound only as long as it keeps to it.
+        asm volatile("s_waitcnt vmcnt(%0)" :: "n"(LOADS) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
 #pragma unroll
