@@ -71,11 +71,11 @@ static int parts_for(long long wgs, int units, long long resident, int fixed) {
   return best;
 }
 
-// Row tiles of a workgroup of cross_dq.hip, at most 32: the fewest within 5 % of the shortest rounds over the `resident` places, if what a workgroup
-// begins and ends with takes `fixed` of a row tile: half of one (512 keys) where it has a compute unit for itself, next to nothing where two
-// fill each other's waits.
-static int chunk_for(long long bh, int tiles, long long resident, double fixed) {
-  auto cost = [&](int c) { return (double)((bh * ((tiles + c - 1) / c) + resident - 1) / resident) * (c + fixed); };
+// Row tiles of a workgroup of cross_dq.hip with 128 channels, at most 32: the fewest within 5 % of the shortest rounds over the `resident` places, as what
+// a workgroup begins and ends with takes half of a row tile (512 keys) where it has a compute unit for itself.  With 64 channels, where two fill each
+// other's waits, that is next to nothing, and one row tile is never more than 5 % behind.
+static int chunk_for(long long bh, int tiles, long long resident) {
+  auto cost = [&](int c) { return (double)((bh * ((tiles + c - 1) / c) + resident - 1) / resident) * (c + 0.5); };
   const int most = tiles < 32 ? tiles : 32;
   double best = cost(1);
   for (int c = 2; c <= most; ++c) best = cost(c) < best ? cost(c) : best;
@@ -123,8 +123,8 @@ hipError_t launch_cross_backward(CrossArgs a, const isa_cross_problem& p, hipStr
     a.items = c.dq_items;
     a.parts = c.dq_parts;
     a.chunk = 1;
-    if (!f32 && c.dq_parts == 1) {
-      a.chunk = chunk_for(bh, c.dq_items, (p.D == 64 ? 2ll : 1ll) * N_XCD * cus_per_xcd(), p.D == 64 ? 0.05 : 0.5);
+    if (!f32 && p.D == 128 && c.dq_parts == 1) {
+      a.chunk = chunk_for(bh, c.dq_items, (long long)N_XCD * cus_per_xcd());
       a.items = (c.dq_items + a.chunk - 1) / a.chunk;
     }
     a.total = bh * a.items * c.dq_parts;

@@ -103,9 +103,6 @@ template <int D> struct FragAt {
   }
 };
 // `at`: FragAt's place plus the LDS address of the sub-tile (a multiple of 256 bytes)
-template <int D> __device__ __forceinline__ bf16x8 frag_rows(uint32_t at, int ks) {
-  return *(__attribute__((address_space(3))) const bf16x8*)(uintptr_t)(at ^ (64u * (uint32_t)ks));
-}
 template <int D> __device__ __forceinline__ bf16x8 frag_tr(uint32_t at, int ct) {
   const uint32_t p = at ^ (32u * (uint32_t)ct);
   const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_ptr)(uintptr_t)p);
@@ -147,7 +144,7 @@ __device__ __forceinline__ uint32_t opaque(uint32_t x) {
   return x;
 }
 
-// The valid keys of the 64 (or `span`) from key0 on, one bit each
+// The valid keys of the 64 from key0 on that lie before `end`, one bit each
 __device__ __forceinline__ unsigned long long valid_keys(const uint8_t* mask_row, int key0, int end, int lane) {
   const int key = key0 + lane;
   bool ok = key < end;
