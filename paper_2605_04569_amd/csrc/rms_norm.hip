@@ -3,7 +3,7 @@
 //   h = x + residual,  r = 1 / sqrt(mean(h^2) + eps),  y = h r w;     8 bits: s = max |y| / 448,  y8 = e4m3(y / s)
 //   g = w dy,  n = h r:  dx = r (g - n mean(g n)) + dh,  dw = sum over rows of dy n
 //
-// Bound by memory: every element is loaded once, a row stays in registers between the sums and the outputs.  LPR lanes share a
+// Bound by memory: every element is loaded once, a row stays in registers between the sums and the outputs (up to 8192 channels: see by_size).  LPR lanes share a
 // row (8 lanes to 1024), each holds NV chunks of 16 bytes of it; a workgroup takes rows in turn, with the next row's loads in
 // flight while it sums the present one, and keeps the weight in registers.  Chunks are loaded at the alignment of an element (the
 // chip's vector loads need no more), so that odd row lengths and strides take the same path; the last chunk of a row whose
@@ -372,8 +372,10 @@ __global__ __launch_bounds__(1024) void k_norm_dw(const float* partial, int n, i
   else reinterpret_cast<__bf16*>(dw)[o] = (__bf16)(float)t;
 }
 
-// Lanes to a row and chunks to a lane: few enough chunks that a row's working set stays in registers beside the next row's loads.
-template <typename F> hipError_t by_size(int chunks, F f) {
+// Lanes to a row and chunks to a lane: few enough chunks that a row's working set stays in registers beside the next row's loads, up to 8192 channels.
+// Beyond, 1024 threads leave 128 registers a lane, and some of what a lane holds goes through scratch memory (bytes a lane, forward / 8 bits / backward):
+// bf16 to 16 384 channels 0 / 0 / 92, to 32 768 0 / 28 / 632; fp32 to 16 384 0 / 0 / 220, to 32 768 240 / 256 / 1100.
+template <typename T, typename F> hipError_t by_size(int chunks, F f) {
 #define ISA_NORM(LPR, NV) return f(std::integral_constant<int, LPR>(), std::integral_constant<int, NV>())
   if (chunks <= 8) ISA_NORM(8, 1);
   if (chunks <= 16) ISA_NORM(16, 1);
@@ -385,8 +387,12 @@ template <typename F> hipError_t by_size(int chunks, F f) {
   if (chunks <= 768) ISA_NORM(256, 3);
   if (chunks <= 1024) ISA_NORM(256, 4);
   if (chunks <= 2048) ISA_NORM(1024, 2);
-  if (chunks <= 4096) ISA_NORM(1024, 4);
-  ISA_NORM(1024, 8);
+  if constexpr (Row<T>::E == 8) {                        // (4096 chunks are 32 768 channels)
+    ISA_NORM(1024, 4);
+  } else {
+    if (chunks <= 4096) ISA_NORM(1024, 4);
+    ISA_NORM(1024, 8);
+  }
 #undef ISA_NORM
 }
 template <typename T> bool streamed(const NormArgs& a) { return a.C % Row<T>::E == 0 && a.rows * a.C * (long long)sizeof(T) >= STREAM_BYTES; }
@@ -413,7 +419,7 @@ int norm_backward_workgroups(const isa_norm_problem* p) {
 
 template <typename T> static hipError_t launch_t(const NormArgs& a, bool eight, hipStream_t st) {
   const int chunks = chunks_of(a.C, Row<T>::E == 8 ? ISA_BF16 : ISA_F32);
-  return by_size(chunks, [&](auto lpr, auto nv) -> hipError_t {
+  return by_size<T>(chunks, [&](auto lpr, auto nv) -> hipError_t {
     constexpr int L = decltype(lpr)::value, N = decltype(nv)::value;
     // Many short turns where the rows are streamed (5120 channels, 8 / 16 / 32 workgroups to a compute unit: 245 / 238 / 230 us, in 8 bits 213 / 207 / 199), fewer
     // loads of the weight where they are few (4096 rows: 25 / 30 / 30)
@@ -433,7 +439,7 @@ hipError_t launch_rms_norm(const NormArgs& a, int dtype, bool eight, hipStream_t
 }
 
 template <typename T> static hipError_t launch_bwd_t(const NormArgs& a, int wgs, hipStream_t st) {
-  return by_size(chunks_of(a.C, Row<T>::E == 8 ? ISA_BF16 : ISA_F32), [&](auto lpr, auto nv) -> hipError_t {
+  return by_size<T>(chunks_of(a.C, Row<T>::E == 8 ? ISA_BF16 : ISA_F32), [&](auto lpr, auto nv) -> hipError_t {
     constexpr int L = decltype(lpr)::value, N = decltype(nv)::value;
     const dim3 grid((unsigned)wgs), blk(threads_of(L));
     by_mode<T>(a, [&](auto mode) { hipLaunchKernelGGL((k_rms_norm_bwd<T, L, N, decltype(mode)::value>), grid, blk, 0, st, a); });
