@@ -23,6 +23,7 @@ struct NormArgs {
   long long sx, sr, sh, sy, sdy, sdh;
 };
 
+bool norm_streams(const NormArgs& a, int dtype, bool eight);  // whether rows go past the caches; looks at the pointers that are set and the sizes
 int norm_backward_workgroups(const isa_norm_problem* p);     // rows of `partial`
 hipError_t launch_rms_norm(const NormArgs& a, int dtype, bool eight, hipStream_t st);
 hipError_t launch_rms_norm_backward(const NormArgs& a, int dtype, int wgs, void* d_weight, hipStream_t st);

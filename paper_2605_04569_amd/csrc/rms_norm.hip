@@ -53,10 +53,12 @@ template <> struct Row<float> {
 };
 
 // How a row's chunks are loaded and stored.  WHOLE: all of them whole chunks, through the caches; TAIL: the last one element by element; STREAMED:
-// whole chunks past the caches, for tensors of STREAM_BYTES or more each, which the caches do not keep for the next kernel anyway (65 520 x 5120 bf16: 8
-// bits 463 -> 444 us, training step 1211 -> 1178; 15 600 x 5120 in 8 bits 108 -> 100; stores alone streamed 459, 1199, 105; loads alone are slower).
+// whole chunks past the caches, where a call's tensors are STREAM_BYTES or more together, the size of the cache in front of the memory: it then keeps little
+// of them for the next kernel anyway.  Chains projection -> norm -> projection of rows of 5120 bf16, us, through the caches / streamed, by the size of one
+// tensor: with the residual (four tensors) 54 MB 159 / -, 66 MB 193 / 184, 130 MB 353 / 343, 512 MB 1438 / 1402; without (two) 66 MB 124 / 135, 96 MB
+// 174 / 189, 130 MB 245 / 235; 8 bits with the residual 96 MB 249 / 238; backward with dh (five) 54 MB 149 / 146, 130 MB 325 / 308.
 enum Mode { WHOLE, TAIL, STREAMED };
-constexpr long long STREAM_BYTES = 64ll << 20;
+constexpr long long STREAM_BYTES = 256ll << 20;
 
 // Chunk c of a row of C elements; zeros past its end.
 template <typename T, Mode M> __device__ __forceinline__ u32x4 load_chunk(const T* row, int c, int C) {
@@ -395,16 +397,23 @@ template <typename T, typename F> hipError_t by_size(int chunks, F f) {
   }
 #undef ISA_NORM
 }
-template <typename T> bool streamed(const NormArgs& a) { return a.C % Row<T>::E == 0 && a.rows * a.C * (long long)sizeof(T) >= STREAM_BYTES; }
-template <typename T, typename F> void by_mode(const NormArgs& a, F f) {
+template <typename T, typename F> void by_mode(const NormArgs& a, bool eight, F f) {
   if (a.C % Row<T>::E != 0) f(std::integral_constant<Mode, TAIL>());
-  else if (streamed<T>(a)) f(std::integral_constant<Mode, STREAMED>());
+  else if (norm_streams(a, Row<T>::E == 8 ? ISA_BF16 : ISA_F32, eight)) f(std::integral_constant<Mode, STREAMED>());
   else f(std::integral_constant<Mode, WHOLE>());
 }
 int slots_of(int chunks) { return chunks <= 8 ? 32 : chunks <= 16 ? 16 : chunks <= 32 ? 8 : chunks <= 128 ? 4 : 1; }
 int chunks_of(int C, int dtype) { return dtype == ISA_BF16 ? (C + 7) / 8 : (C + 3) / 4; }
 
 }  // namespace
+
+bool norm_streams(const NormArgs& a, int dtype, bool eight) {
+  const long long size = dtype == ISA_BF16 ? 2 : 4;
+  long long bytes = eight ? 1 : size;                      // of an element of every tensor: y or dx, then those that the call has
+  for (const void* t : {a.x, a.residual, (const void*)a.h, a.dy, a.dh})
+    if (t) bytes += size;
+  return a.C % (16 / size) == 0 && a.rows * a.C * bytes >= STREAM_BYTES;
+}
 
 int norm_backward_workgroups(const isa_norm_problem* p) {
   const int chunks = chunks_of(p->channels, p->dtype);
@@ -423,9 +432,9 @@ template <typename T> static hipError_t launch_t(const NormArgs& a, bool eight, 
     constexpr int L = decltype(lpr)::value, N = decltype(nv)::value;
     // Many short turns where the rows are streamed (5120 channels, 8 / 16 / 32 workgroups to a compute unit: 245 / 238 / 230 us, in 8 bits 213 / 207 / 199), fewer
     // loads of the weight where they are few (4096 rows: 25 / 30 / 30)
-    const long long slots = threads_of(L) / L, wide = streamed<T>(a) ? 32 : 8, most = (L > 256 ? 2 : wide) * (long long)N_XCD * cus_per_xcd(), n = (a.rows + slots - 1) / slots;
+    const long long slots = threads_of(L) / L, wide = norm_streams(a, Row<T>::E == 8 ? ISA_BF16 : ISA_F32, eight) ? 32 : 8, most = (L > 256 ? 2 : wide) * (long long)N_XCD * cus_per_xcd(), n = (a.rows + slots - 1) / slots;
     const dim3 grid((unsigned)(n < most ? n : most)), blk(threads_of(L));
-    by_mode<T>(a, [&](auto mode) {
+    by_mode<T>(a, eight, [&](auto mode) {
       constexpr Mode M = decltype(mode)::value;
       if (eight) hipLaunchKernelGGL((k_rms_norm<T, L, N, M, true>), grid, blk, 0, st, a);
       else hipLaunchKernelGGL((k_rms_norm<T, L, N, M, false>), grid, blk, 0, st, a);
@@ -442,7 +451,7 @@ template <typename T> static hipError_t launch_bwd_t(const NormArgs& a, int wgs,
   return by_size<T>(chunks_of(a.C, Row<T>::E == 8 ? ISA_BF16 : ISA_F32), [&](auto lpr, auto nv) -> hipError_t {
     constexpr int L = decltype(lpr)::value, N = decltype(nv)::value;
     const dim3 grid((unsigned)wgs), blk(threads_of(L));
-    by_mode<T>(a, [&](auto mode) { hipLaunchKernelGGL((k_rms_norm_bwd<T, L, N, decltype(mode)::value>), grid, blk, 0, st, a); });
+    by_mode<T>(a, false, [&](auto mode) { hipLaunchKernelGGL((k_rms_norm_bwd<T, L, N, decltype(mode)::value>), grid, blk, 0, st, a); });
     return hipGetLastError();
   });
 }
