@@ -318,6 +318,7 @@ int isa_cross_attention(const isa_cross_problem* p, const void* q, const void* k
 /* Gradients of isa_cross_attention with respect to q, k and v.  q, k, v, kv_len, key_mask: as given to it; out, lse: as written by it;
  * d_out: the gradient of out.  (rowsum(d_out * out) is that of an output that is not rounded: bf16 works out by how much that of `out` is off.)
  * All of dq, dk and dv is written: keys and values that are not valid get zeros, and queries without a valid key too.
+ * dk and dv may both be NULL (states that need no gradient): their launch is left out.
  * The gradient of a key head is the sum over the query heads that share it.  The outputs share no memory with the inputs or
  * with each other. */
 int isa_cross_attention_backward(const isa_cross_problem* p, const void* q, const void* k, const void* v, const int32_t* kv_len,

@@ -490,7 +490,10 @@ def isa_cross_attention(q, k, v, out, kv_len=None, key_mask=None, scale=None, ls
 
 
 def isa_cross_attention_backward(q, k, v, out, lse, d_out, dq, dk, dv, kv_len=None, key_mask=None, scale=None, workspace=None):
-    cp = _cross_problem(q, k, v, out, scale, d_out, dq, dk, dv)
+    """dk and dv: None together where the states need no gradient."""
+    if (dk is None) != (dv is None):
+        raise ValueError("dk and dv come together")
+    cp = _cross_problem(q, k, v, out, scale, d_out, dq, *((k, v) if dk is None else (dk, dv)))
     _check_lse(q, lse)
     masks = _cross_masks(q, k, kv_len, key_mask)
     ws, n = _cross_workspace(cp, 1, workspace, q.device)

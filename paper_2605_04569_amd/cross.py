@@ -64,9 +64,11 @@ class _CrossAttentionFunction(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, d_out):
         q, k, v, out, lse, kv_len, key_mask = ctx.saved_tensors
-        dq, dk, dv = _like(q), _like(k), _like(v)
+        need_q, need_k, need_v = ctx.needs_input_grad[:3]
+        dq = _like(q)                                  # (and the rows' deltas, which dk and dv want)
+        dk, dv = (_like(k), _like(v)) if need_k or need_v else (None, None)
         B.isa_cross_attention_backward(q, k, v, out, lse, _layout(d_out), dq, dk, dv, kv_len, key_mask, ctx.scale)
-        return dq, dk, dv, None, None, None
+        return dq if need_q else None, dk if need_k else None, dv if need_v else None, None, None, None
 
 
 def cross_attention(q, k, v, kv_len=None, key_mask=None, scale=None):

@@ -142,7 +142,7 @@ hipError_t launch_cross_backward(CrossArgs a, const isa_cross_problem& p, hipStr
     }
     if (e != hipSuccess) return e;
   }
-  if (p.S_k > 0) {
+  if (p.S_k > 0 && a.dk) {
     a.items = c.kv_items;
     a.parts = c.kv_parts;
     a.total = bh * c.kv_items * c.kv_parts;

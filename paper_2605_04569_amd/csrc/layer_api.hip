@@ -143,11 +143,12 @@ int isa_cross_attention_backward(const isa_cross_problem* p, const void* q, cons
                                  size_t workspace_bytes, void* hip_stream) {
   int rc = check_cross(p);
   if (rc != ISA_OK) return rc;
-  if (!read_strides(p->d_out) || !write_strides(p, p->dq, p->H) || !write_strides(p, p->dk, p->H_kv) || !write_strides(p, p->dv, p->H_kv))
-    return ISA_ERR_SHAPE;
+  const bool states = dk || dv;                          // neither: dq alone is worked out
+  if (!read_strides(p->d_out) || !write_strides(p, p->dq, p->H)) return ISA_ERR_SHAPE;
+  if (states && (!write_strides(p, p->dk, p->H_kv) || !write_strides(p, p->dv, p->H_kv))) return ISA_ERR_SHAPE;
   if (p->B == 0 || (p->S_q == 0 && p->S_k == 0)) return ISA_OK;
   if (p->S_q > 0 && (!q || !out || !lse || !d_out || !dq)) return ISA_ERR_NULL;
-  if (p->S_k > 0 && (!k || !v || !dk || !dv)) return ISA_ERR_NULL;
+  if (p->S_k > 0 && (!k || !v || (states && (!dk || !dv)))) return ISA_ERR_NULL;
   if (!all_aligned16(q, k, v, out, d_out, dq, dk, dv) || !whole(lse, ISA_F32)) return ISA_ERR_SHAPE;
   const void* ins[] = {q, k, v, out, d_out};
   const void* outs[] = {dq, dk, dv};
