@@ -307,7 +307,8 @@ size_t isa_cross_workspace_bytes(const isa_cross_problem* p, int backward);
  * kv_len: NULL, or device int32 [B]: key j of batch item b is valid for j < kv_len[b] (taken as 0 / S_k where it is below / above).
  * key_mask: NULL, or device bytes [B][key_mask_stride]: and key_mask[b][j] != 0 (0 and 1, as torch's bool, or any other byte).
  * What keys and values that are not valid hold has no influence, infinities and NaN included; nothing past S_k is read.
- * A row without a valid key gets zeros.  lse: NULL, or device fp32 [B, H, S_q] contiguous: the natural logarithm of the sum of the
+ * A row without a valid key gets zeros; no other row is taken for one: a score counts whatever its size, except that in bf16 a row whose largest
+ * score is beyond 2^30 in size may come out as NaN, as a row does whose scores are all minus infinity.  lse: NULL, or device fp32 [B, H, S_q] contiguous: the natural logarithm of the sum of the
  * exponentials, minus infinity for a row without a valid key; for the backward pass.
  * bf16: products of bf16 numbers with fp32 sums; the softmax weights are rounded to bf16 for the product with v and
  * normalised by the sum of the rounded ones.  fp32: fp32 products throughout.  No atomics: results are reproducible. */

@@ -5,6 +5,8 @@
 
 namespace isa {
 
+constexpr float LOWEST = -3.402823466e38f;    // the running maximum before the first key: no finite score is below it
+
 // What the kernels get of an isa_cross_problem.  The query heads that share a key head are one sequence of `rows` = group * S_q rows:
 // row r of key head hk is query r % S_q of head hk * group + r / S_q.
 struct CrossArgs {
@@ -23,7 +25,7 @@ struct CrossArgs {
   int parts;                        // every item runs as this many workgroups, each over its share of the keys (dk, dv: of the queries)
   long long total;                  // work items * parts of all (batch item, key head)s
   // partial results of the parts: sums before normalisation [item][part][rows of a tile][D] and, per row, {maximum, sum of the weights
-  // as multiplied, their sum before they were rounded, unused}; bf16 dq: sums of dS' k and of P k [item][part][row][2][D], {sum of dS', ..}
+  // as multiplied, their sum before they were rounded, 1 if the part had a valid key}; bf16 dq: sums of dS' k and of P k [item][part][row][2][D], {sum of dS', ..}
   float* part_o;
   float4* part_ml;
   // backward

@@ -87,7 +87,7 @@ __global__ __launch_bounds__(256, 2) void k_cross_rows_f32(CrossArgs a) {
   const int use = ok ? row : tile0, head = hk * a.group + use / a.Sq, query = use % a.Sq;
   f32x4 own_q[CT], own_o[CT];
   load_own<D>(reinterpret_cast<const float*>(a.q) + at_row(a.sq, b, head, query), q, true, own_q);
-  float neg_m = -M_INIT, l = 0.f, nd = 0.f;              // BWD: neg_m is minus the log-sum-exp
+  float neg_m = -LOWEST, l = 0.f, nd = 0.f;              // BWD: neg_m is minus the log-sum-exp
   if constexpr (BWD) {
     f32x4 o[CT];
     load_own<D>(reinterpret_cast<const float*>(a.d_out) + at_row(a.sdo, b, head, query), q, true, own_o);
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(256, 2) void k_cross_rows_f32(CrossArgs a) {
   const float* const k_head = reinterpret_cast<const float*>(a.k) + at_row(a.sk, b, hk, 0);
   const float* const v_head = reinterpret_cast<const float*>(a.v) + at_row(a.sv, b, hk, 0);
   TileRegs<D> rk, rv;
-  unsigned long long valid = 0, valid_next = 0;
+  unsigned long long valid = 0, valid_next = 0, seen = 0;
   auto fetch = [&](int t) __attribute__((always_inline)) {
     valid_next = valid_keys(mask_row, t * FT, min(n_keys, t * FT + FT), lane);
     const bool live = (valid_next >> (tid >> 3)) & 1ull;
@@ -126,6 +126,7 @@ __global__ __launch_bounds__(256, 2) void k_cross_rows_f32(CrossArgs a) {
   if (t_begin < t_end) fetch(t_begin);
   for (int t = t_begin; t < t_end; ++t) {
     valid = valid_next;
+    seen |= valid;
     __syncthreads();
     rk.put(kt_, tid);
     rv.put(vt_, tid);
@@ -182,16 +183,18 @@ __global__ __launch_bounds__(256, 2) void k_cross_rows_f32(CrossArgs a) {
   if (a.parts > 1) {
     const long long at = (slot * a.parts + part) * 64 + wave * 16 + r16;
     store_own<D>(acc, 1.0f, a.part_o + at * D, q);
-    if (!BWD && q == 0) a.part_ml[at] = make_float4(-neg_m, l, l, 0.f);
+    if (!BWD && q == 0) a.part_ml[at] = make_float4(-neg_m, l, l, seen ? 1.f : 0.f);
     return;
   }
   if (!ok) return;
   if constexpr (BWD) {
     store_own<D>(acc, a.scale, reinterpret_cast<float*>(a.dq) + at_row(a.sdq, b, head, query), q);
   } else {
-    store_own<D>(acc, l == 0.f ? 0.f : 1.0f / l, reinterpret_cast<float*>(a.out) + at_row(a.so, b, head, query), q);
+    // (a valid key whose score is minus infinity, and no other: no weights to speak of)
+    const float none = seen ? __builtin_nanf("") : 0.f;
+    store_own<D>(acc, l == 0.f ? none : 1.0f / l, reinterpret_cast<float*>(a.out) + at_row(a.so, b, head, query), q);
     if (a.lse && q == 0)
-      a.lse[((long long)b * a.H + head) * a.Sq + query] = l > 0.f ? 0.6931471805599453f * (log2f(l) - neg_m) : l == 0.f ? -INFINITY : l;
+      a.lse[((long long)b * a.H + head) * a.Sq + query] = l > 0.f ? 0.6931471805599453f * (log2f(l) - neg_m) : l == 0.f ? (seen ? none : -INFINITY) : l;
   }
 }
 

@@ -36,7 +36,7 @@ struct RowState {
   f32x4 l;                          // the lane's share of the sum of the rounded weights (all elements alike)
   float lu;                         // of the weights before they are rounded
 };
-__device__ __forceinline__ RowState row_state() { return RowState{-M_INIT, M_INIT + RESCALE_TAU, f32x4{0.f, 0.f, 0.f, 0.f}, 0.f}; }
+__device__ __forceinline__ RowState row_state() { return RowState{-LOWEST, LOWEST, f32x4{0.f, 0.f, 0.f, 0.f}, 0.f}; }
 
 __device__ __forceinline__ float top_of(const f32x4 (&s)[2]) {
   float m = -INFINITY;
@@ -73,8 +73,11 @@ template <bool LSE> __device__ __forceinline__ bf16x8 weights(const f32x4 s0, co
   return __builtin_bit_cast(bf16x8, make_uint4(p[0], p[1], p[2], p[3]));
 }
 
-__device__ __forceinline__ float natural_lse(float m, float lu) {      // m: log2 domain
-  return lu > 0.f ? 0.6931471805599453f * (m + __log2f(lu)) : (lu == 0.f ? -INFINITY : lu);
+// The weights of a row with a valid key add up to 2^-RESCALE_TAU at least, unless its scores are so large (2^31) that their rounding takes the weights
+// out of range: NaN then, so that the row is not taken for one without a key.
+__device__ __forceinline__ float inverse_of(float l, bool keys) { return l != 0.f ? 1.0f / l : keys ? __builtin_nanf("") : 0.f; }
+__device__ __forceinline__ float natural_lse(float m, float lu, bool keys) {      // m: log2 domain
+  return lu > 0.f ? 0.6931471805599453f * (m + __log2f(lu)) : lu == 0.f ? (keys ? __builtin_nanf("") : -INFINITY) : lu;
 }
 
 }  // namespace
@@ -116,12 +119,13 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossArgs a) {
   auto load_v = [&](int u, uint32_t stage, uint32_t w) __attribute__((always_inline)) {
     lv.issue(uniform_ptr(v_head + (long long)u * NK * a.sv.t), lds0 + (NST + stage) * (uint32_t)TILE, wave, lane, w);
   };
-  uint32_t w[5] = {0, 0, 0, 0, 0};                         // key bits of tiles u .. u + 4; a tile behind the last has none
+  uint32_t w[5] = {0, 0, 0, 0, 0}, seen = 0;               // key bits of tiles u .. u + 4; a tile behind the last has none.  seen: of all tiles
   if (n > 0) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (i < n) {
         w[i] = bits.of(t_begin + i);
+        seen |= w[i];
         load_k(i, i, w[i]);
         if (i < 2) load_v(i, i, w[i]);
       }
@@ -228,6 +232,7 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossArgs a) {
     __syncthreads();
     if (u + 3 < n) { w[3] = bits.of(t_begin + u + 3); load_k(u + 3, (PAR + 3) % NST, w[3]); }
     if (u + 4 < n) { w[4] = bits.of(t_begin + u + 4); load_k(u + 4, PAR, w[4]); }
+    seen |= w[3] | w[4];
     if (u + 1 < n) load_v(u + 1, (PAR + 1) % NST, w[1]);
     if (u + 2 < n) load_v(u + 2, (PAR + 2) % NST, w[2]);
     step(s_even, s_odd, (PAR + 1) % NST, (PAR + 3) % NST, w[0]);
@@ -287,13 +292,13 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossArgs a) {
       const long long row = ((long long)slot * a.parts + part) * 128 + wave * 32 + 16 * qt + r16;
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) *reinterpret_cast<f32x4*>(a.part_o + row * D + 16 * ct + 4 * q) = acc[qt][ct];
-      if (q == 0) a.part_ml[row] = make_float4(-st[qt].neg_m, l, lu, 0.f);
+      if (q == 0) a.part_ml[row] = make_float4(-st[qt].neg_m, l, lu, seen ? 1.f : 0.f);
       continue;
     }
     const RowOf row(a, hk, tile0, (int)opaque((uint32_t)(wave * 32 + 16 * qt + r16)));      // (worked out again: nothing of it stays in registers)
     const long long o = at_row(a.so, b, row.head, row.query);
-    store_row<D>(acc[qt], l == 0.f ? 0.f : 1.0f / l, reinterpret_cast<uint16_t*>(a.out) + o, q, row.ok);
-    if (LSE && q == 0 && row.ok) a.lse[((long long)b * a.H + row.head) * a.Sq + row.query] = natural_lse(-st[qt].neg_m, lu);
+    store_row<D>(acc[qt], inverse_of(l, seen != 0), reinterpret_cast<uint16_t*>(a.out) + o, q, row.ok);
+    if (LSE && q == 0 && row.ok) a.lse[((long long)b * a.H + row.head) * a.Sq + row.query] = natural_lse(-st[qt].neg_m, lu, seen != 0);
   }
 }
 
@@ -352,7 +357,7 @@ __global__ __launch_bounds__(256, 2) void k_cross_narrow(CrossArgs a) {
   for (int ct = 0; ct < CT; ++ct) acc[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
   const f32x4 zero4 = {0.f, 0.f, 0.f, 0.f};
 
-  unsigned long long valid = 0, valid_next = 0;
+  unsigned long long valid = 0, valid_next = 0, seen = 0;
   int t = t_begin + wave;
   if (t < t_end) {
     valid_next = valid_keys(mask_row, t * NK, min(n_keys, t * NK + NK), lane);
@@ -360,6 +365,7 @@ __global__ __launch_bounds__(256, 2) void k_cross_narrow(CrossArgs a) {
   }
   for (int buf = 0; t < t_end; t += 4, buf ^= 1) {
     valid = valid_next;
+    seen |= valid;
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");      // this tile is here, and the reads of the one before it are over
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
@@ -392,15 +398,15 @@ __global__ __launch_bounds__(256, 2) void k_cross_narrow(CrossArgs a) {
   float* const mine = reinterpret_cast<float*>(stage);
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) *reinterpret_cast<f32x4*>(mine + r16 * D + 16 * ct + 4 * q) = acc[ct];
-  if (q == 0) ml[wave][r16] = make_float4(-st.neg_m, l, lu, 0.f);
+  if (q == 0) ml[wave][r16] = make_float4(-st.neg_m, l, lu, seen ? 1.f : 0.f);
   __syncthreads();
   // 16 threads to a row, D / 16 channels each
   const int row = tid >> 4, c0 = (tid & 15) * (D / 16);
   if (row >= a.rows) return;
-  float m = M_INIT;
+  float m = LOWEST;
 #pragma unroll
   for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w][row].x);
-  float o[D / 16], sum = 0.f, sum_u = 0.f;
+  float o[D / 16], sum = 0.f, sum_u = 0.f, keys = 0.f;
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) o[i] = 0.f;
 #pragma unroll
@@ -409,6 +415,7 @@ __global__ __launch_bounds__(256, 2) void k_cross_narrow(CrossArgs a) {
     const float f = __builtin_amdgcn_exp2f(e.x - m);
     sum = fmaf(e.y, f, sum);
     sum_u = fmaf(e.z, f, sum_u);
+    keys = fmaxf(keys, e.w);
     const float* from = reinterpret_cast<const float*>(lds + w * 2 * TILE) + row * D + c0;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) o[i] = fmaf(from[i], f, o[i]);
@@ -417,17 +424,17 @@ __global__ __launch_bounds__(256, 2) void k_cross_narrow(CrossArgs a) {
     const long long at_part = ((long long)bh * a.parts + part) * 16 + row;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) a.part_o[at_part * D + c0 + i] = o[i];
-    if (c0 == 0) a.part_ml[at_part] = make_float4(m, sum, sum_u, 0.f);
+    if (c0 == 0) a.part_ml[at_part] = make_float4(m, sum, sum_u, keys);
     return;
   }
   const int oh = hk * a.group + row / a.Sq, oq = row % a.Sq;
-  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  const float inv = inverse_of(sum, keys != 0.f);
   const long long to = at_row(a.so, b, oh, oq) + c0;
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
     reinterpret_cast<__bf16*>(a.out)[to + i] = (__bf16)(o[i] * inv);
   }
-  if (LSE && c0 == 0) a.lse[((long long)b * a.H + oh) * a.Sq + oq] = natural_lse(m, sum_u);
+  if (LSE && c0 == 0) a.lse[((long long)b * a.H + oh) * a.Sq + oq] = natural_lse(m, sum_u, keys != 0.f);
 }
 
 // out = sum_p O_p 2^(m_p - m) / sum_p l_p 2^(m_p - m), m = max_p m_p.  D / 4 threads take a row of a part; `split` such groups share a row's parts
@@ -443,7 +450,7 @@ __global__ __launch_bounds__(256) void k_cross_merge(CrossArgs a, int tile_rows,
   const bool in = bh < a.B * a.Hkv;
   const int b = bh % a.B, hk = bh / a.B;
   const long long base = ((long long)bh * a.items + row / tile_rows) * a.parts * tile_rows + row % tile_rows;
-  float m = M_INIT, l = 0.f, lu = 0.f;
+  float m = LOWEST, l = 0.f, lu = 0.f, keys = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   if (in) {
     // four parts' loads in flight
@@ -455,7 +462,7 @@ __global__ __launch_bounds__(256) void k_cross_merge(CrossArgs a, int tile_rows,
         const long long at = base + (long long)min(p0 + i * split, a.parts - 1) * tile_rows;
         e[i] = a.part_ml[at];
         x[i] = *reinterpret_cast<const f32x4*>(a.part_o + at * D + c);
-        if (p0 + i * split >= a.parts) e[i] = make_float4(M_INIT, 0.f, 0.f, 0.f);
+        if (p0 + i * split >= a.parts) e[i] = make_float4(LOWEST, 0.f, 0.f, 0.f);
       }
       const float m_new = fmaxf(fmaxf(fmaxf(m, e[0].x), fmaxf(e[1].x, e[2].x)), e[3].x), f0 = __builtin_amdgcn_exp2f(m - m_new);
       l *= f0;
@@ -468,12 +475,13 @@ __global__ __launch_bounds__(256) void k_cross_merge(CrossArgs a, int tile_rows,
         const float f = __builtin_amdgcn_exp2f(e[i].x - m);
         l = fmaf(e[i].y, f, l);
         lu = fmaf(e[i].z, f, lu);
+        keys = fmaxf(keys, e[i].w);
         o += x[i] * f;
       }
     }
   }
   if (split > 1) {
-    if (c == 0) ml[group] = make_float4(m, l, lu, 0.f);
+    if (c == 0) ml[group] = make_float4(m, l, lu, keys);
     sums[group][c >> 2] = o;
     __syncthreads();
     if (share) return;
@@ -483,16 +491,17 @@ __global__ __launch_bounds__(256) void k_cross_merge(CrossArgs a, int tile_rows,
       l = l * f0 + e.y * f1;
       lu = lu * f0 + e.z * f1;
       o = o * f0 + sums[group + g][c >> 2] * f1;
+      keys = fmaxf(keys, e.w);
       m = m_new;
     }
   }
   if (!in) return;
-  o *= l == 0.f ? 0.f : 1.0f / l;
+  o *= inverse_of(l, keys != 0.f);
   const int head = hk * a.group + row / a.Sq, query = row % a.Sq;
   const long long to = at_row(a.so, b, head, query) + c;
   if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + to) = bf16x4_of(o);
   else *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + to) = o;
-  if (a.lse && c == 0) a.lse[((long long)b * a.H + head) * a.Sq + query] = natural_lse(m, lu);
+  if (a.lse && c == 0) a.lse[((long long)b * a.H + head) * a.Sq + query] = natural_lse(m, lu, keys != 0.f);
 }
 
 CrossPlan cross_forward_plan(const isa_cross_problem& p) {
