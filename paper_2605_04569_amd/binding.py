@@ -401,17 +401,14 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
-def _recorded(*ts):
-    """Whether a call has to go through its torch.autograd function, because a gradient is wanted, a forward-mode derivative may be carried
-    along (which the function refuses) or the call is being traced (which records the function): the library's own calls on
-    raw addresses are seen by neither."""
-    if torch._C._get_tracing_state() is not None or getattr(forward_ad, "_current_level", 0) >= 0:
-        return True
-    if torch.is_grad_enabled():
-        for t in ts:
-            if t is not None and t.requires_grad:
-                return True
-    return False
+_tracing_state = torch._C._get_tracing_state
+
+
+def _recorded():
+    """Whether a call has to go through its torch.autograd function though no gradient is wanted: a forward-mode derivative may be carried along
+    (which the function refuses) or the call is being traced (which records the function); both see nothing of the library's own
+    calls on raw addresses."""
+    return _tracing_state() is not None or getattr(forward_ad, "_current_level", 0) >= 0
 
 
 def _strides(t):

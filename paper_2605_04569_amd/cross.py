@@ -85,7 +85,7 @@ def cross_attention(q, k, v, kv_len=None, key_mask=None, scale=None):
     if kv_len is not None or key_mask is not None:
         kv_len, key_mask = _masks(q, k, kv_len, key_mask)
     scale = float(shape_q[3] ** -0.5 if scale is None else scale)
-    if B._recorded(q, k, v):
+    if (torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad)) or B._recorded():
         return _CrossAttentionFunction.apply(q, k, v, kv_len, key_mask, scale)
     q, k, v = _layout(q), _layout(k), _layout(v)
     return B.isa_cross_attention(q, k, v, _like(q), kv_len, key_mask, scale)

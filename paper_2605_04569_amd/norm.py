@@ -95,7 +95,8 @@ class _ResidualRMSNormFunction(torch.autograd.Function):
 def residual_rms_norm(x, weight=None, residual=None, eps=1e-6):
     """y, or (y, h) with a residual; differentiable in x, weight and residual."""
     _check(x, weight, residual)
-    if B._recorded(x, weight, residual):
+    if (torch.is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad) or
+                                     (residual is not None and residual.requires_grad))) or B._recorded():
         return _ResidualRMSNormFunction.apply(x, weight, residual, eps)
     y, h, _, order, _, _ = _forward(x, None if weight is None else weight.contiguous(), residual, eps, False)
     return _back(y, order) if residual is None else (_back(y, order), _back(h, order))
@@ -106,7 +107,9 @@ def residual_rms_norm_8bit(x, weight=None, residual=None, eps=1e-6, group=0):
     dimension of 1) or of its 128 channels (group 128).  For inference: not differentiable."""
     _check(x, weight, residual)
     B._require(group in (0, 128) and (group == 0 or x.shape[-1] % 128 == 0), "group is 0, or 128 and divides the channels")
-    return (_ResidualRMSNorm8Function.apply if B._recorded() else _eight_bit)(x, weight, residual, eps, group)
+    if B._recorded():
+        return _ResidualRMSNorm8Function.apply(x, weight, residual, eps, group)
+    return _eight_bit(x, weight, residual, eps, group)
 
 
 def _eight_bit(x, weight, residual, eps, group):
