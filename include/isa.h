@@ -351,7 +351,8 @@ int isa_rms_norm(const isa_norm_problem* p, const void* x, const void* residual,
                  float* rstd, void* hip_stream);
 
 /* The same with y in 8 bits (e4m3, the OCP format with largest value 448): scale = max |y| / 448 over a row or a group of 128
- * channels (at least 2^-126; 1 where the maximum is 0), y8 = y / scale rounded to nearest even.  scales: device fp32 [rows][channels / group] contiguous
+ * channels (at least 2^-126; 1 where the maximum is 0), y8 = y / scale rounded to nearest even.  (448 and the scale divide by their
+ * fp32 reciprocals: a scale is within 2^-23 of the quotient, and a y8 whose quotient is as near to the middle of two may be either.)  scales: device fp32 [rows][channels / group] contiguous
  * ([rows] for group 0).  stride_y is that of y8, in bytes; y8 shares no memory with the inputs or h. */
 int isa_rms_norm_8bit(const isa_norm_problem* p, const void* x, const void* residual, const void* weight, void* h, void* y8,
                       float* scales, void* hip_stream);

@@ -305,7 +305,8 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossArgs a) {
 // STREAM: keys and values are loaded past the caches, which is quicker where those cannot keep them from call to call (more than 256 MB, the size of the
 // cache in front of the memory): 8 rows over 16 384 states of 8 heads, 537 MB 103 -> 89 us (6.0 TB/s), 1074 MB 185 -> 161 (6.7).  268 MB: 46 -> 48 us if
 // they were read the call before, 56 -> 49 if not.
-// States that several batch items or heads share (a stride of 0) count once.
+// States that several batch items or heads share (a stride of 0) count once, as they are read from memory once (8 requests of 5 rows a head on one document
+// of 67 or 134 MB: 51 and 86 us a call, past the caches 51 and 87).
 constexpr long long KEPT_BYTES = 256ll << 20;
 template <int D, bool LSE, bool STREAM>
 __global__ __launch_bounds__(256, 2) void k_cross_narrow(CrossArgs a) {
